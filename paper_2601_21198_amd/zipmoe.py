@@ -500,8 +500,7 @@ class Layer:
         self._values = values
         args = _moe_args(x, ids, weights, out, scales, residual, values // hidden if hidden else 0)
         names = (ctypes.c_int32 * max(1, len(expert_ids)))(*expert_ids)
-        rc = (_lib or lib()).zm_layer_moe(self._handle, names, len(expert_ids), args, workspace.data_ptr(),
-                                          workspace.numel() * workspace.element_size(), stream)
+        rc = (_lib or lib()).zm_layer_moe(self._handle, names, len(expert_ids), args, *_workspace(workspace), stream)
         if rc != OK:
             raise ZipMoEError(rc, "zm_layer_moe")
 
@@ -565,6 +564,13 @@ def _flat(t, shape, what, dtypes):
     if t.dtype not in dtypes:
         raise TypeError(f"{what}: {t.dtype}, not {' or '.join(map(str, dtypes))}")
     return t.data_ptr()
+
+
+def _workspace(t):
+    """(address, bytes) of a workspace: what a call that writes into it is told of its size has to be there"""
+    if not t.is_cuda or not t.is_contiguous():
+        raise ValueError("workspace: not a contiguous tensor in device memory")
+    return t.data_ptr(), t.numel() * t.element_size()
 
 
 def _byte_types():
@@ -636,7 +642,7 @@ def route(x, weight, ids, weights, workspace, bias=None, token_mask=None, logits
     po = _flat(weights, (tokens, top_k), "weights", f32)
     pl = _flat(logits, (tokens, experts), "logits", f32) if logits is not None else 0
     rc = L.zm_route(_ROUTE_ARGS.pack(px, pw, pb, pm, pi, po, pl, sx, sw, tokens, hidden, experts, top_k, kind, bool(renormalise), scale),
-                    workspace.data_ptr(), workspace.numel() * workspace.element_size(), stream)
+                    *_workspace(workspace), stream)
     if rc != OK:
         raise ZipMoEError(rc, "zm_route")
 
@@ -699,7 +705,7 @@ class Experts:
         if x.shape[-1] != self.hidden:
             raise ValueError(f"x: rows of {x.shape[-1]} values, not {self.hidden}")
         rc = L.zm_moe(self._tensors, self._ids, self.n_experts, _moe_args(x, ids, weights, out, scales, residual, self.intermediate),
-                      workspace.data_ptr(), workspace.numel() * workspace.element_size(), stream)
+                      *_workspace(workspace), stream)
         if rc != OK:
             raise ZipMoEError(rc, "zm_moe")
 
