@@ -561,7 +561,7 @@ typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
 // 16 bytes per lane from memory to LDS, lane after lane from `to` on.
 __device__ __forceinline__ void to_lds(uint32_t to, uint32_t offset, i32x4 from, uint32_t step)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(to), "v"(offset), "s"(from), "s"(step) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(to), "v"(offset), "s"(from), "s"(step) : "memory", "m0");
 }
 // All but the last n requests have arrived, for every wave of the workgroup, and nobody reads the stage before any more.
 template <int n>
