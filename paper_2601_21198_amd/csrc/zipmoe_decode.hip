@@ -1107,8 +1107,11 @@ struct Multiplier {
             for (int i = 0; i < 4; ++i) d = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, ws[i]), __builtin_bit_cast(bf16x2, xs[i]), d, false);
             if constexpr (kRest) {
                 __builtin_memcpy(xs, to->x[j] + rest + col, 16);
+                float more = 0.0f;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) d = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, ws[i]), __builtin_bit_cast(bf16x2, xs[i]), d, false);
+                for (int i = 0; i < 4; ++i) more = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, ws[i]), __builtin_bit_cast(bf16x2, xs[i]), more, false);
+                // an infinite value of the matrix times a remainder of zero, or of the other sign, is none of the sum's
+                d += fabsf(d) < INFINITY ? more : 0.0f;
             }
 #pragma unroll
             for (int r = 0; r < kRows; ++r) to->s[r][j] += row == static_cast<uint32_t>(r) ? d : 0.0f;

@@ -161,6 +161,7 @@ __device__ __forceinline__ f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c) { return __bu
 __device__ __forceinline__ float silu(float g) { return g / (1.0f + expf(-g)); }
 // Where the result is rounded to bf16: 2^-22 (2 + |g|) from it, in a third of the instructions.
 __device__ __forceinline__ float silu_short(float g) { return g * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504f * g)); }
+__device__ __forceinline__ bool finite(float v) { return fabsf(v) < INFINITY; }
 __device__ __forceinline__ uint16_t bits(__bf16 v) { return __builtin_bit_cast(uint16_t, v); }
 __device__ __forceinline__ float of_bf16(uint16_t w) { return __builtin_bit_cast(float, static_cast<uint32_t>(w) << 16); }
 
@@ -445,7 +446,7 @@ __global__ void __launch_bounds__(64 * kFirstWaves, kTiles == 1 ? 4 : 2) zm_moe_
                 const uint64_t at = static_cast<uint64_t>(pair - 1) * c.intermediate + row0 + r;
                 c.h[at] = bits(most);
                 const float rest = h - static_cast<float>(most);
-                c.h_rest[at] = bits(static_cast<__bf16>(fabsf(rest) < INFINITY ? rest : 0.0f));      // most tells of what is not finite
+                c.h_rest[at] = bits(static_cast<__bf16>(finite(rest) ? rest : 0.0f));      // most tells of what is not finite
             }
         }
     }
@@ -500,10 +501,13 @@ __global__ void __launch_bounds__(64 * kSecondWaves, 4) zm_moe_few_second_kernel
             const uint32_t pair = kAhead ? n.pair : pairs.pair(s, c, n.slot, 16 * t + Lines::line(lane));
             if (!kAhead && __builtin_amdgcn_ballot_w64(pair != 0) == 0) continue;
             const Columns h = kAhead ? n.h : columns_at(pair, n.k);
-            f32x4 sum = {};
+            f32x4 sum = {}, rest = {};
 #pragma unroll
-            for (int i = 0; i < 4; ++i) sum = mfma(n.w.v[i], h.most.v[i], sum), sum = mfma(n.w.v[i], h.rest.v[i], sum);
-            // an infinite weight times the zeros of a token that did not choose the expert is none of the token's
+            for (int i = 0; i < 4; ++i) sum = mfma(n.w.v[i], h.most.v[i], sum), rest = mfma(n.w.v[i], h.rest.v[i], rest);
+            // an infinite weight times the zeros of a token that did not choose the expert is none of the token's, nor is one times a remainder
+            // of zero, or of the other sign: where the first parts give no finite sum they give the result
+#pragma unroll
+            for (int r = 0; r < 4; ++r) sum[r] += finite(sum[r]) ? rest[r] : 0.0f;
             if (pair) y[t] += sum;
         }
     };

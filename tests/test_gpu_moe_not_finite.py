@@ -1,0 +1,54 @@
+"""What zm_moe and zm_layer_moe make of weights and scales that are not finite: what the formula gives, in calls of any number of tokens and from compressed
+experts too."""
+import math
+
+import pytest
+import torch
+
+from test_gpu_moe import Case, layer_forward, layer_of
+
+pytestmark = pytest.mark.gpu
+# tokens, top_k, compressed: one token, a lane per pair, a table of pairs, two tiles of columns, many tokens, large tiles; products while decoding, decoded first
+CALLS = [(1, 2, False), (6, 2, False), (12, 8, False), (32, 4, False), (130, 2, False), (1500, 2, False), (1, 2, True), (2, 2, True), (4, 2, True), (8, 3, True), (40, 2, True)]
+
+
+def case(tokens, top_k, kind="bf16"):
+    """experts 3 and 6 have a token each at least"""
+    c = Case(tokens, 256, 256, 9, top_k, kind)
+    c.ids[0, :2] = torch.tensor([3, 6], dtype=torch.int32)
+    return c
+
+
+def call(c, compressed):
+    return layer_forward(c, layer_of(c, 2048, 512), c.names) if compressed else c.forward()
+
+
+@pytest.mark.parametrize("tokens,top_k,compressed", CALLS)
+def test_infinite_weights_of_down(tokens, top_k, compressed):
+    """an output of an expert's tokens is infinite, by the sign that h has"""
+    c = case(tokens, top_k)
+    c.w[2][3, 5, 40] = math.inf
+    c.w[2][6, 7, 41] = -math.inf
+    got = call(c, compressed).double()
+    want, bound = c.exact(few=False)
+    infinite = torch.isinf(want)
+    assert torch.any(infinite) and not torch.any(torch.isnan(want))
+    assert torch.equal(got[infinite], want[infinite])
+    assert torch.all(((got - want).abs() <= bound)[~infinite])
+
+
+@pytest.mark.parametrize("tokens,top_k,compressed", CALLS)
+def test_one_significant_bit_meets_infinity(tokens, top_k, compressed):
+    """h is a power of two: nothing is left of it behind its first bf16 part"""
+    c = case(tokens, top_k)
+    c.x.fill_(0)
+    c.x[:, 0] = 1.0
+    c.w[0][:, :, 0] = 128.0                     # silu(128) is 128: exp(-128) is below half a step of 1
+    c.w[1][:, :, 0] = 0.5
+    c.weights.fill_(0.25)
+    c.w[2][3, 5, 40] = math.inf
+    c.w[2][3, 9, 40] = -math.inf
+    got = call(c, compressed)
+    mine = (c.ids == 3).any(1)
+    assert torch.all(got[mine][:, 5] == math.inf) and torch.all(got[mine][:, 9] == -math.inf)
+    assert torch.all(torch.isfinite(got[~mine])) and torch.all(torch.isfinite(got[:, 10:]))
