@@ -603,7 +603,7 @@ int zm_sched_lower_bounds(const zm_sched_task *tasks, int n_tasks, const double 
 #define ZM_BF16 0
 #define ZM_FP16 1
 #define ZM_FP32 2
-#define ZM_MXFP8 3        /* e4m3 bytes with one e8m0 scale byte (2^(b-127)) per 32 consecutive values of a row, the last group may be short */
+#define ZM_MXFP8 3        /* e4m3 bytes with one e8m0 scale byte (2^(b-127), 255 is NaN) per 32 consecutive values of a row, the last group may be short */
 #define ZM_SCALE_GROUP 32
 
 /* Root-mean-square norm behind a residual addition:

@@ -130,7 +130,8 @@ __device__ __forceinline__ bf16x8 eight(const uint16_t *row, uint32_t k, uint32_
     return u.v;
 }
 
-// The same of an e4m3 row with its scales: four significant bits times a power of two is a bf16 value as it is.
+// The same of an e4m3 row with its scales: four significant bits times a power of two is a bf16 value as it is, from 2^-130 (below, bf16's
+// steps are 2^-133) up to 2^128 (infinity).  Scale byte 255 is e8m0's NaN.
 __device__ __forceinline__ bf16x8 eight_scaled(const uint8_t *row, const uint8_t *scales, uint32_t k, uint32_t width)
 {
     union { uint8_t b[8]; uint32_t w[2]; } q;
@@ -143,8 +144,14 @@ __device__ __forceinline__ bf16x8 eight_scaled(const uint8_t *row, const uint8_t
         for (uint32_t i = 0; i < 8; ++i)
             if (k + i < width) q.b[i] = row[k + i];
     }
-    const int b = static_cast<int>(scales[k / 32]) - 127;
+    const uint8_t scale = scales[k / 32];
+    const int b = static_cast<int>(scale) - 127;
     bf16x8 v;
+    if (scale == 255) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = static_cast<__bf16>(NAN);
+        return v;
+    }
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(q.w[i], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(q.w[i], true);

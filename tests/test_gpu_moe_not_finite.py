@@ -52,3 +52,18 @@ def test_one_significant_bit_meets_infinity(tokens, top_k, compressed):
     mine = (c.ids == 3).any(1)
     assert torch.all(got[mine][:, 5] == math.inf) and torch.all(got[mine][:, 9] == -math.inf)
     assert torch.all(torch.isfinite(got[~mine])) and torch.all(torch.isfinite(got[:, 10:]))
+
+
+@pytest.mark.parametrize("tokens,top_k,compressed", CALLS)
+def test_a_scale_that_is_not_a_number(tokens, top_k, compressed):
+    """e8m0's 255, over zeros too"""
+    c = case(tokens, top_k, "mx8")
+    clean = call(c, compressed).clone()
+    bad = sorted({0, tokens - 1})
+    for t in bad:
+        c.scales[t, 2] = 255
+        c.x[t, 64:96] = torch.zeros(32, device="cuda").to(torch.float8_e4m3fn)
+    got = call(c, compressed)
+    assert torch.all(torch.isnan(c.scales.view(torch.float8_e8m0fnu).float()[bad, 2]))
+    others = [t for t in range(tokens) if t not in bad]
+    assert torch.all(torch.isnan(got[bad])) and torch.equal(got[others], clean[others])
