@@ -285,13 +285,12 @@ int launch_route(const Route &p, bool few, hipStream_t stream)
 {
     Route q = p;
     void *args[] = {&q};
-    if (!few)
-        return hipLaunchKernel(p.n_experts > 16 ? reinterpret_cast<const void *>(&zm_route_tile_kernel<T, kTight, 2>) : reinterpret_cast<const void *>(&zm_route_tile_kernel<T, kTight, 1>),
-                               dim3((p.n_tokens + 15) / 16), dim3(1024), args, 0, stream) == hipSuccess ? ZM_OK : ZM_E_HIP;
     const uint32_t across = (p.n_experts + 4 * kWaveExperts - 1) / (4 * kWaveExperts);
-    for (uint32_t done = 0; done < p.n_tokens;) {                           // a grid's y axis has 16 bits
+    // a grid has less than 2^32 threads along an axis, 1024 for a tile's 16 tokens; its y axis has 16 bits
+    const uint32_t most = few ? 65535u : 1u << 25;
+    for (uint32_t done = 0; done < p.n_tokens;) {
         q = p;
-        const uint32_t n = p.n_tokens - done < 65535u ? p.n_tokens - done : 65535u;
+        const uint32_t n = p.n_tokens - done < most ? p.n_tokens - done : most;
         const uint32_t size = static_cast<uint32_t>(sizeof(T));
         q.x = static_cast<const uint8_t *>(p.x) + done * p.x_stride * size;
         q.n_tokens = n;
@@ -299,11 +298,16 @@ int launch_route(const Route &p, bool few, hipStream_t stream)
         if (q.logits) q.logits += static_cast<uint64_t>(done) * p.n_experts;
         if (q.token_mask) q.token_mask += done;
         q.sums += static_cast<uint64_t>(done) * p.n_experts;
+        done += n;
+        if (!few) {
+            const void *fn = p.n_experts > 16 ? reinterpret_cast<const void *>(&zm_route_tile_kernel<T, kTight, 2>) : reinterpret_cast<const void *>(&zm_route_tile_kernel<T, kTight, 1>);
+            if (hipLaunchKernel(fn, dim3((n + 15) / 16), dim3(1024), args, 0, stream) != hipSuccess) return ZM_E_HIP;
+            continue;
+        }
         const bool one = n < 4;
         const void *fn = one ? reinterpret_cast<const void *>(&zm_route_logits_kernel<T, kTight, 1>) : reinterpret_cast<const void *>(&zm_route_logits_kernel<T, kTight, 4>);
         if (hipLaunchKernel(fn, dim3(across, one ? n : (n + 3) / 4), dim3(256), args, 0, stream) != hipSuccess) return ZM_E_HIP;
         if (hipLaunchKernel(reinterpret_cast<const void *>(&zm_route_choose_kernel), dim3(n), dim3(64), args, 0, stream) != hipSuccess) return ZM_E_HIP;
-        done += n;
     }
     return ZM_OK;
 }
