@@ -120,12 +120,17 @@ int launch(const void *fn, dim3 grid, void *call, hipStream_t stream)
 bool takes_products(const zm_layer &layer, const int32_t *ids, int n, const zm_moe_args &a, size_t &sums)
 {
     const uint64_t pairs = static_cast<uint64_t>(a.n_tokens) * static_cast<uint64_t>(a.top_k);
-    if (n == 0 || a.n_tokens > kProductVectors || pairs > kProductPairs || a.hidden % 8 || a.intermediate % 8) return false;
-    const uint32_t W = layer.infos[3 * ids[0]].stream_values;
+    if (n == 0) return false;
+    const uint32_t W = layer.infos[3 * ids[0]].stream_values, hidden = static_cast<uint32_t>(a.hidden), intermediate = static_cast<uint32_t>(a.intermediate);
+    if (!product_fits(hidden, intermediate, W, a.n_tokens, pairs)) return false;
+    bool long_codes = false;
     for (int i = 0; i < n; ++i)
-        for (int m = 0; m < 3; ++m)
-            if (layer.infos[3 * ids[i] + m].stream_values != W) return false;
-    if (W > kProductStream || product_rows(a.hidden, W) > kProductRows || product_rows(a.intermediate, W) > kProductRows) return false;
+        for (int m = 0; m < 3; ++m) {
+            const zm_tensor_info &info = layer.infos[3 * ids[i] + m];
+            if (info.stream_values != W) return false;
+            long_codes = long_codes || info.max_len > 8;
+        }
+    if (!product_pays(hidden, intermediate, W, long_codes, a.n_tokens, pairs, static_cast<uint64_t>(n))) return false;
     const uint64_t streams = (layer.infos[3 * ids[0]].n_values + W - 1) / W;
     sums = sizeof(float) * pairs * (2 * (streams + a.intermediate) + streams + a.hidden);
     return true;

@@ -6,10 +6,9 @@
 #include <cstdint>
 
 #include "zipmoe.h"
+#include "zipmoe_product_rule.h"
 
 namespace zipmoe {
-
-constexpr int kProductPairs = 64, kProductVectors = 8;     // pairs of a call, vectors that one matrix meets
 
 // Which vectors meet which matrix, and where the sums go.
 struct ProductCall {
@@ -24,15 +23,7 @@ struct ProductCall {
     uint32_t pieces;
 };
 
-// The piece of row r that lies in stream g has number g + r: both grow by one where either changes.  Most rows that a stream touches:
-inline uint32_t product_rows(uint32_t width, uint32_t stream_values)
-{
-    return stream_values % width == 0 ? stream_values / width : width % stream_values == 0 ? 1u : stream_values / width + 2u;
-}
-constexpr uint32_t kProductRows = 4, kProductStream = 8192;      // most rows and values of a stream
-
-// Multiplies n matrices; matrix i is number i % per_expert of expert ids[i / per_expert].  Checked by the caller: addresses, and that
-// product_rows is at most kProductRows and streams have at most kProductStream values.
+// Multiplies n matrices; matrix i is number i % per_expert of expert ids[i / per_expert].  Checked by the caller: addresses, and product_fits.
 int product_launch(const void *const *blobs, const uint64_t *const *tables, const zm_tensor_info *const *infos, const int32_t *ids, int n, int per_expert,
                    const ProductCall &call, hipStream_t stream);
 

@@ -1,12 +1,13 @@
 """The kernels of zm_moe and zm_layer_moe that calls of few tokens take, each reached on purpose: tables of more than 64 pairs, two tiles of columns, products of
 compressed experts in every width of vectors and rows.  Bounds are those of test_gpu_moe, with h in two bf16 parts: up to 32 tokens and 512 pairs."""
-import math
+from concurrent.futures import ThreadPoolExecutor
 
+import numpy as np
 import pytest
 import torch
 
 from paper_2601_21198_amd import zipmoe as zm
-from test_gpu_moe import Case, layer_forward, layer_of
+from test_gpu_moe import Case, layer_forward
 
 pytestmark = pytest.mark.gpu
 
@@ -91,13 +92,27 @@ def rows_of_a_stream(width, stream):
     return stream // width if stream % width == 0 else 1 if width % stream == 0 else stream // width + 2
 
 
-def multiplied(c, stream):
-    return (c.tokens <= 8 and c.tokens * c.top_k <= 64 and c.hidden % 8 == 0 and c.inter % 8 == 0 and stream <= 8192 and
-            max(rows_of_a_stream(c.hidden, stream), rows_of_a_stream(c.inter, stream)) <= 4)
+def multiplied(tokens, hidden, inter, top_k, named, stream, long_codes):
+    """the rule of zipmoe_product_rule.h"""
+    rows = rows_of_a_stream(hidden, stream), rows_of_a_stream(inter, stream)
+    if tokens > 8 or tokens * top_k > 64 or hidden % 8 or inter % 8 or not 1024 <= stream <= 8192 or max(rows) > 4:
+        return False
+    many = sum(rows) > 6
+    if tokens > 4 and (stream != 4096 or (many and long_codes)):
+        return False
+    return 2 * tokens * top_k <= named * (5 if stream < 2048 or many or (stream > 4096 and long_codes) else 8)
 
 
-# hidden, inter, chunk, stream: one and two rows, four; rows that straddle streams; last streams that are cut off inside a tile; rows of several streams
-WIDTHS = [(256, 512, 4096, 512), (128, 256, 4096, 512), (200, 176, 2048, 512), (352, 360, 4096, 1024), (1376, 1368, 4096, 4096), (1024, 520, 1024, 512), (1536, 512, 2048, 1024)]
+def layer_of(c, chunk, stream, max_len=8):
+    words = [m[e].view(torch.int16).reshape(-1).cpu().numpy().view(np.uint16) for e in range(c.n) for m in c.w]
+    with ThreadPoolExecutor(8) as pool:
+        blobs = list(pool.map(lambda w: zm.compress(w, chunk, stream, max_len)[0], words))
+    return zm.Layer([blobs[i: i + 3] for i in range(0, len(blobs), 3)])
+
+
+def reaches(c, layer, named):
+    info = [layer.tensor_info(e, m) for e in named for m in range(3)]
+    return multiplied(c.tokens, c.hidden, c.inter, c.top_k, len(named), info[0].stream_values, any(i.max_len > 8 for i in info))
 
 
 def fill(c, values):
@@ -112,14 +127,20 @@ def fill(c, values):
             m.fill_(0.03125)
 
 
-@pytest.mark.parametrize("values", ["short", "long", "raw", "one"])
-@pytest.mark.parametrize("hidden,inter,chunk,stream", WIDTHS)
-@pytest.mark.parametrize("tokens", [1, 2, 4, 7])
+# hidden, inter, chunk, stream: one to four rows a stream, rows that straddle streams, last streams that are cut off inside a tile, rows of several streams
+WIDTHS = [(512, 1024, 4096, 1024), (256, 512, 2048, 1024), (352, 360, 4096, 1024), (1032, 2048, 4096, 2048), (1536, 512, 2048, 1024), (2048, 1024, 4096, 4096), (1024, 2048, 16384, 4096),
+          (1376, 1368, 4096, 4096)]
+PRODUCTS = [(tokens, *w, values) for w in WIDTHS for values in ("short", "long", "raw", "one") for tokens in (1, 2, 4, 5, 7)
+            if multiplied(tokens, w[0], w[1], 3, 6, w[3], values != "short")]
+assert {t for t, *_ in PRODUCTS} == {1, 2, 4, 5, 7} and all(any(p[1:5] == w for p in PRODUCTS) for w in WIDTHS)
+
+
+@pytest.mark.parametrize("tokens,hidden,inter,chunk,stream,values", PRODUCTS)
 def test_products(tokens, hidden, inter, chunk, stream, values):
-    c = Case(tokens, hidden, inter, 4, 3, "mx8" if tokens == 4 else "bf16", residual=tokens != 2)
-    assert multiplied(c, stream)
+    c = Case(tokens, hidden, inter, 6, 3, "mx8" if tokens == 4 else "bf16", residual=tokens != 2)
     fill(c, values)
     layer = layer_of(c, chunk, stream, 8 if values == "short" else 12)
+    assert reaches(c, layer, c.names)
     got = layer_forward(c, layer, c.names)
     c.check(got, few=True)
     assert torch.equal(layer_forward(c, layer, c.names), got)
@@ -127,46 +148,54 @@ def test_products(tokens, hidden, inter, chunk, stream, values):
 
 def test_products_of_long_streams():
     c = Case(3, 4096, 2736, 1, 1)
-    assert multiplied(c, 8192)
-    c.check(layer_forward(c, layer_of(c, 16384, 8192), c.names), few=True)
+    layer = layer_of(c, 16384, 8192)
+    assert reaches(c, layer, c.names)
+    c.check(layer_forward(c, layer, c.names), few=True)
 
 
-@pytest.mark.parametrize("tokens,experts", [(8, 9), (8, 50), (5, 45)])
-def test_products_of_64_pairs_and_many_experts(tokens, experts):
-    """more matrices than a launch takes, short and long codes among them"""
-    c = Case(tokens, 256, 256, experts, 8, zipf=0.3)
-    assert multiplied(c, 512)
-    gen = torch.Generator().manual_seed(experts)
-    for m in c.w:
-        m[1::2] *= torch.exp(torch.randn(m[1::2].shape, generator=gen) * 2 - 4).cuda()
-    layer = layer_of(c, 4096, 512, 12)
+@pytest.mark.parametrize("tokens,experts,top_k,hidden,inter,stream", [(4, 50, 16, 512, 256, 1024), (1, 100, 64, 512, 256, 1024), (8, 26, 8, 1024, 1024, 4096)])
+def test_products_of_64_pairs_and_many_experts(tokens, experts, top_k, hidden, inter, stream):
+    """more matrices than a launch takes; in the smaller ones short and long codes side by side"""
+    c = Case(tokens, hidden, inter, experts, top_k, zipf=0.3)
+    if stream == 1024:
+        gen = torch.Generator().manual_seed(experts)
+        for m in c.w:
+            m[1::2] *= torch.exp(torch.randn(m[1::2].shape, generator=gen) * 2 - 4).cuda()
+    layer = layer_of(c, 4096, stream, 12 if stream == 1024 else 8)
+    assert reaches(c, layer, c.names)
+    c.check(layer_forward(c, layer, c.names), few=True)                     # some of which nobody chose
     c.check(layer_forward(c, layer, sorted(set(c.ids.reshape(-1).tolist()))), few=True)
-    c.check(layer_forward(c, layer, c.names), few=True)                     # and those that nobody chose
+
+
+def small(tokens, kind="bf16", dropped=0.0):
+    """a case that multiplies, and its layer's geometry"""
+    return (Case(tokens, 512, 1024, 9, 4, kind, dropped=dropped, zipf=1.0, pad=8), 2048, 1024) if tokens <= 4 else (Case(tokens, 2048, 1024, 9, 2, kind, dropped=dropped, zipf=1.0, pad=8), 4096, 4096)
 
 
 @pytest.mark.parametrize("tokens", [1, 2, 3, 8])
 def test_products_of_some_experts(tokens):
-    c = Case(tokens, 256, 512, 9, 4, dropped=0.3, zipf=1.0, pad=3)
-    assert multiplied(c, 512)
-    names = [8, 1, 3, 0]
+    c, chunk, stream = small(tokens, dropped=0.3)
+    names = [8, 1, 3, 0, 6]
     c.ids[c.ids == 3] = 5                                                   # nobody wants 3; 5 is not named
     for m in c.w:
         m[3] = float("nan")
         m[5] = float("nan")
-    layer = layer_of(c, 2048, 512)
+    layer = layer_of(c, chunk, stream)
+    assert reaches(c, layer, names)
     c.check(layer_forward(c, layer, names), names, few=True)
-    c.ids[:, 1] = c.ids[:, 0] = 1                                           # twice, once with another between
-    c.ids[:, 3] = 1
+    c.ids[:, 1] = c.ids[:, 0] = 1                                           # twice, in the longer lists with others between
+    c.ids[:, -1] = 1
     c.check(layer_forward(c, layer, names), names, few=True)
     c.ids[:] = -1
     assert torch.equal(layer_forward(c, layer, names), c.residual)
     assert torch.equal(layer_forward(c, layer, []), c.residual)
 
 
-@pytest.mark.parametrize("tokens", [2, 8])
+@pytest.mark.parametrize("tokens", [2, 4, 8])
 def test_products_with_a_token_that_is_not_finite(tokens):
-    c = Case(tokens, 256, 512, 4, 2)
-    layer = layer_of(c, 2048, 512)
+    c, chunk, stream = small(tokens)
+    layer = layer_of(c, chunk, stream)
+    assert reaches(c, layer, c.names)
     clean = layer_forward(c, layer, c.names).clone()
     c.x[1, 7] = float("nan")
     got = layer_forward(c, layer, c.names)
@@ -177,14 +206,15 @@ def test_products_with_a_token_that_is_not_finite(tokens):
 @pytest.mark.parametrize("kind", ["bf16", "mx8"])
 @pytest.mark.parametrize("tokens", [1, 2, 4, 8])
 def test_products_in_a_graph(tokens, kind):
-    c = Case(tokens, 256, 512, 5, 2, kind)
-    layer = layer_of(c, 2048, 512)
-    ws, out = c.workspace(layer.moe_workspace_bytes(5, tokens, 2, 256)), torch.empty(tokens, 256, dtype=torch.bfloat16, device="cuda")
+    c, chunk, stream = small(tokens, kind)
+    layer = layer_of(c, chunk, stream)
+    assert reaches(c, layer, c.names)
+    ws, out = c.workspace(layer.moe_workspace_bytes(9, tokens, c.top_k, c.hidden)), torch.empty(tokens, c.hidden, dtype=torch.bfloat16, device="cuda")
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
         layer.moe(c.names, c.x, c.ids, c.weights, out, ws, scales=c.scales, residual=c.residual, stream=torch.cuda.current_stream().cuda_stream)
     for k in range(3):
-        other = Case(tokens, 256, 512, 5, 2, kind, seed=k + 1)
+        other = Case(tokens, c.hidden, c.inter, 9, c.top_k, kind, seed=k + 1, pad=8)
         c.x.copy_(other.x), c.ids.copy_(other.ids), c.weights.copy_(other.weights)
         if kind == "mx8":
             c.scales.copy_(other.scales)
