@@ -659,7 +659,8 @@ int zm_route(const zm_route_args *args, void *workspace, size_t workspace_bytes,
  * [intermediate, hidden], down [hidden, intermediate], as the decode calls and zm_cache_fetch leave them):
  *   out_t = residual_t + sum_j weights_tj * down_e (silu(gate_e x_t) * (up_e x_t)),   e = ids_tj
  * Products are summed in 32 bits and the sum over a token's experts is rounded once; between the two products the activations
- * of a call of many tokens are rounded to bf16.  The order of every sum is fixed: equal calls give equal bits. */
+ * are held in two bf16 parts (16 significant bits) in calls of up to 32 tokens with up to 512 pairs of a token and an expert, and rounded to
+ * bf16 in larger ones.  The order of every sum is fixed: equal calls give equal bits. */
 typedef struct zm_moe_args {
     const void *x;             /* DEVICE [n_tokens, hidden]: ZM_BF16 or ZM_MXFP8                          */
     const void *scales;        /* DEVICE bytes [n_tokens, ceil(hidden / 32)] for ZM_MXFP8, else NULL      */

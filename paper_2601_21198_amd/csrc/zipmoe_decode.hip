@@ -1138,8 +1138,10 @@ __device__ __forceinline__ float wave_total(float v)
 }
 
 // A wave decodes a stream as the decode kernels do and multiplies it instead of storing it: 1.35 bytes a value are moved, where a decode and a
-// product that reads what it wrote move 5.35.  Bound by the wait for the vectors behind every tile and by the vector unit (half of its time); two, three,
-// four, five and six waves per SIMD: 139, 125, 119, 162 and 197 us for eight tokens through 8 of 24 experts of 1024 x 2048 (fewer registers spill).
+// product that reads what it wrote move 5.35.  Bound by the wait for the vectors behind every tile and by the vector unit (half of its time).  The sums of
+// one and two vectors fit into the registers that four waves per SIMD leave; of four vectors with three or four rows 4 to 48 registers go to scratch memory, of eight 39 (two rows)
+// to 231 (four), with long codes 73 to 415, and two waves per SIMD, which spill least, are no faster: two, three, four, five and six waves: 139, 125, 119, 162 and 197 us for
+// eight tokens through 8 of 24 experts of 1024 x 2048.  Which calls this is worth it for: zipmoe_product_rule.h.
 template <bool kLong, int kWaves, int kVectors, int kRows, bool kRest>
 __global__ void __launch_bounds__(64 * kWaves, 4) zm_layer_product_kernel(const ProductLaunch P)
 {

@@ -4,16 +4,17 @@
 //
 // A pair is a token and one of its experts, numbered t * top_k + j.
 //
-// Few tokens (up to 32, with up to 512 pairs) are bound by the matrices' bytes (experts of 1408 x 2048, one token through 4: 69 MB in 21.4 us; of 1024 x
-// 2048, 16 tokens through 8 of 64: 470 MB in 116 us): two launches, each of which finds out for itself which experts
+// Few tokens (up to 32, with up to 512 pairs) are bound by the matrices' bytes (experts of 1408 x 2048, one token through 4: 69 MB in 21.2 us where they stay cached, 24.3 where not; of 1024 x
+// 2048, 16 tokens through 8 of 64: 470 MB in 122 us): two launches, each of which finds out for itself which experts
 // somebody chose and streams their matrices from memory into matrix instructions, once.
 //   few_first    16 rows of gate and up of one expert times the tokens that chose it; the weighted h in two bf16 parts
 //   few_second   16 rows of down of every chosen expert times h; an expert's column for a token is its weighted h, so one
 //                accumulator sums over experts
 // Many tokens are bound by the matrix cores: the pairs are put in the order of their experts, and tiles of pairs multiply 256 rows.  4096 tokens
-// through 2 of 8 experts of 4096 x 14336 take 2.4 ms, 1207 TFLOP/s (a plain library product of these sizes 1374).
+// through 2 of 8 experts of 4096 x 14336 take 2.4 ms, 1190 TFLOP/s (a plain library product of these sizes 1545 on the same card).
 //   list         one workgroup per expert: its pairs, in order, from the number of pairs with smaller ids on
-//   product      gate and up (h in bf16), then down, in tiles of 128 pairs; wide: in tiles of 256 or 288
+//   product      gate and up, then down, in tiles of 128 pairs; wide: in tiles of 256 or 288.  h is rounded to bf16 once, which the result shows (off by
+//                2.3e-3 of its norm, its own rounding alone by 1.7e-3): a second part would be half as many matrix instructions again
 //   join         residual + the weighted sum over a token's pairs
 //
 // The matrix instruction v_mfma_f32_16x16x32_bf16 multiplies 16 rows of 32 values (lane l: row l % 16, values 8 (l / 16) .. + 7) with 16
@@ -358,7 +359,7 @@ struct FirstTile {
 };
 
 // Tiles of 16 rows (8 for one token) of gate and up of one chosen expert, taken in turn by the workgroups.
-// kTiles: 16 tokens each that the call has at most
+// kTiles: 16 tokens each that the call has at most.  Four waves per SIMD leave 128 registers, of which those for 2 to 16 tokens keep 4 to 8 in scratch memory.
 template <class Pairs, bool kTight, int kTiles, int kParts>
 __global__ void __launch_bounds__(64 * kFirstWaves, kTiles == 1 ? 4 : 2) zm_moe_few_first_kernel(const Call c, const Experts e)
 {
@@ -1002,7 +1003,7 @@ __global__ void __launch_bounds__(256) zm_moe_join_kernel(const Call c, const Id
 
 constexpr uint32_t kUnits = 256;         // compute units
 constexpr uint32_t kFewGrid = 1024;      // workgroups of few_first
-// Pairs per expert from which the large tiles are taken.  us small / large tiles, experts of 4096 x 14336, 128 pairs each 796 / 818, 192 905 / 839,
+// Pairs per expert that the call names from which the large tiles are taken; how they spread over the experts is known on the device only.  us small / large tiles, experts of 4096 x 14336, 128 pairs each 796 / 818, 192 905 / 839,
 // 1024 3216 / 2392; of 2048 x 1024, 128 259 / 287, 192 296 / 291, 512 655 / 595; of 2048 x 1408, 137 318 / 353, 273 574 / 533.
 constexpr uint64_t kWideFrom = 160;
 constexpr uint32_t kFewParts = 4;        // most workgroups that share the rows of few_second

@@ -313,7 +313,7 @@ int launch_route(const Route &p, bool few, hipStream_t stream)
 }
 
 // Whether a call goes without tiles.  A tile's product takes hidden * 16 ceil(n_experts / 16) * 0.17 ns, on as many compute units at once as there are 16
-// tokens; without tiles all of them take part in hidden * n_experts * n_tokens * 0.102 fs, and a second launch takes 3 us.  us without / with tiles:
+// tokens; without tiles all of them take part in hidden * n_experts * n_tokens * 0.102 ps, and a second launch takes 3 us.  us without / with tiles:
 // 64 experts of 2048, 512 tokens 14.1 / 26.0, 2048 35.2 / 26.3; 256 experts, 1024 tokens 60 / 89, 2048 112 / 90; 8 experts of 4096, 1024 tokens
 // 11.2 / 16.3, 4096 21.9 / 18.4; 16 experts of 512, 9 tokens 7.2 / 5.2.
 bool takes_few(int64_t n_tokens, int64_t hidden, int64_t n_experts)
